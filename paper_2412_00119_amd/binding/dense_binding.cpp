@@ -134,6 +134,12 @@ double real(PyObject *o) {
   if (v == -1.0 && PyErr_Occurred()) throw PyError{};
   return v;
 }
+int32_t whole(PyObject *o, const char *what) {
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw PyError{};
+  if (v < 0) refuse("%s is negative", what);
+  return dim32(v, what);
+}
 bool truth(PyObject *o) {
   const int v = PyObject_IsTrue(o);
   if (v < 0) throw PyError{};
@@ -257,29 +263,32 @@ PyObject *qlinear_pack(PyObject *, PyObject *const *a, Py_ssize_t count) {
   });
 }
 
-// qlinear(q, scale, dtype, packed, wscale, bias, n_in) -> out; the layer's own
-// tensors were checked when it was made
+// qlinear(q, scale, dtype, packed, wscale, bias, n_in, n_out) -> out.  The
+// layer's own tensors are attributes that a program can replace: they are checked
+// against its sizes like any other argument.
 PyObject *qlinear(PyObject *, PyObject *const *a, Py_ssize_t count) {
   return guarded([&]() -> PyObject * {
-    arguments(count, 7);
+    arguments(count, 8);
     const at::Tensor &q = tensor(a[0], "q"), &packed = tensor(a[3], "packed"), &wscale = tensor(a[4], "wscale");
     const at::Tensor *scale = tensor_or_none(a[1], "scale"), *bias = tensor_or_none(a[5], "bias");
     if (!THPDtype_Check(a[2])) refuse("%s must be a torch dtype", "dtype");
     const at::ScalarType dtype = reinterpret_cast<THPDtype *>(a[2])->scalar_type;
     const int type = type_of(dtype);
     if (type < 0) refuse("%s must be float32, bfloat16 or float16", "dtype");
-    const long long k = PyLong_AsLongLong(a[6]);
-    if (k == -1 && PyErr_Occurred()) throw PyError{};
-    const int64_t ldq = rows(q, "q"), n = q.size(0), m = wscale.size(0);
+    const int32_t k = whole(a[6], "n_in"), m = whole(a[7], "n_out");
+    const int64_t ldq = rows(q, "q"), n = q.size(0);
     const at::Device dev = packed.device();
+    const size_t bytes = bmlp_qlinear_packed_bytes(m, k);
+    if (bytes == 0 || !packed.is_cuda()) refuse("the layer's %s", "sizes are outside the supported ones, or it is not on the GPU");
+    vector(packed, "the layer's packed weights", (int64_t)bytes, dev, at::kByte);
+    float *wsp = floats(&wscale, "the layer's scale", m, dev), *bp = floats(bias, "the layer's bias", m, dev);
     if (q.scalar_type() != at::kChar || q.size(1) != k || q.device() != dev)
       refuse("%s must be int8 rows of the layer's width on its device", "q");
     float *sp = floats(scale, "scale", n, dev);
     const OnDevice on(dev);
     at::Tensor out = make({n, m}, dtype, dev);
-    check(bmlp_qlinear(type, (int32_t)n, (int32_t)m, (int32_t)k, static_cast<const int8_t *>(q.data_ptr()), ldq, sp,
-                       packed.data_ptr(), static_cast<const float *>(wscale.data_ptr()),
-                       bias != nullptr ? static_cast<const float *>(bias->data_ptr()) : nullptr, out.data_ptr(), m, on.stream),
+    check(bmlp_qlinear(type, (int32_t)n, m, k, static_cast<const int8_t *>(q.data_ptr()), ldq, sp, packed.data_ptr(), wsp, bp,
+                       out.data_ptr(), m, on.stream),
           "bmlp_qlinear");
     return THPVariable_Wrap(out);
   });

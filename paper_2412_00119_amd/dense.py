@@ -96,7 +96,7 @@ class QLinear:
 
     def __call__(self, q, scale=None, dtype=torch.bfloat16):
         """q int8 [n][K] with a scale for each row (None: ones) -> [n][N] of dtype."""
-        return _c.qlinear(q, scale, dtype, self.packed, self.scale, self.bias, self.n_in)
+        return _c.qlinear(q, scale, dtype, self.packed, self.scale, self.bias, self.n_in, self.n_out)
 
 
 def distill(z, idx, t, tau: float = 1.0, lse=None, weight=None, grad: bool = True):

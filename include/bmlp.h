@@ -368,7 +368,8 @@ enum { BMLP_TYPE_F32 = 0, BMLP_TYPE_BF16 = 1, BMLP_TYPE_F16 = 2 };
  *             NULL: the values that q stands for.
  * A row whose largest |t| is 2^-118 or less gets q = 0, scale = 0.  A row in
  * which some t is not finite gets q = 0, scale = NaN and y = NaN.  A row
- * whose squares' mean passes the 32-bit range has rstd = 0 and scale = 0.
+ * whose squares' mean passes the 32-bit range has rstd = 0 and scale = 0, and so
+ * has one whose root mean square is 2^-118 or less at eps = 0 (a row of zeros).
  * 1 <= K <= BMLP_MAX_NORM_WIDTH, eps >= 0 and finite. */
 int bmlp_norm_quant(int32_t type, int32_t n, int32_t K, const void *d_x, int64_t ldx, const void *d_res,
                     int64_t ldr, const void *d_weight, int32_t weight_type, float eps, int8_t *d_q, int64_t ldq,

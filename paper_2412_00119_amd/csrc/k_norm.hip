@@ -109,14 +109,31 @@ __device__ __forceinline__ vec_t<float, VEC> load_weight(const void *w, bool f32
 
 constexpr float kTiny = 0x1p-118f;   // 127 / kTiny is still finite
 
+// Squares are summed times p.down, about 1 / K, so that the sum stays in range
+// wherever the mean does.  What a square loses to the range's low end (2^-150 at
+// most) is below 2^-33 of a mean of kSmallMean or more.  Where the mean with eps is
+// smaller, which takes an eps that is (SMALL), a second sum of (h kUp)^2 is used:
+// it has every digit down to h = 2^-149 and stays in range up to means far above.
+// A template parameter, since the second sum spills in the widest shape (1024 x 65536
+// f32 277 us without, 289 with).
+constexpr float kSmallMean = 0x1p-100f, kUp = 0x1p90f;
+template <bool SMALL>
+__device__ __forceinline__ float norm_rstd(float ss, float ss_up, const NormArgs &p) {
+  if (!p.norm) return 1.f;
+  const float mean = ss / ((float)p.K * p.down) + p.eps;
+  if (!SMALL || !(mean < kSmallMean)) return 1.f / sqrtf(mean);   // (NaN too)
+  const float up = ss_up / (float)p.K + p.eps * kUp * kUp;
+  return up > kTiny * kUp * (kTiny * kUp) ? kUp / sqrtf(up) : 0.f;
+}
+
 // NT threads and R vectors of 16 bytes of x per thread to a row; a wave per
 // row (four in a work-group) or a work-group per row.
-template <typename T, int NT, int R>
+template <typename T, int NT, int R, bool SMALL>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_quant_kernel(NormArgs p) {
   constexpr int VEC = 16 / sizeof(T), G = NT < 256 ? 256 / NT : 1, W = NT / 64;
   static_assert(NT == 64 || NT >= 256, "a wave or a whole work-group per row");
   typedef vec_t<float, VEC> fv;
-  __shared__ float s_ss[W];
+  __shared__ float s_ss[W], s_up[SMALL ? W : 1];
   __shared__ uint32_t s_top[W];
   const int g = G > 1 ? (int)threadIdx.x / NT : 0, t = G > 1 ? (int)threadIdx.x % NT : (int)threadIdx.x;
   const int64_t row = (int64_t)blockIdx.x * G + g;
@@ -126,7 +143,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_quant_kernel(NormArg
   const T *r = p.res != nullptr ? static_cast<const T *>(p.res) + row * p.ldr : nullptr;
   T *ho = p.h != nullptr ? static_cast<T *>(p.h) + row * p.ldh : nullptr;
   fv tv[R];
-  float ss = 0.f;
+  float ss = 0.f, ss_up = 0.f;
   uint32_t top = 0u;
   vec_t<T, VEC> xv[R], rv[R];
 #pragma unroll
@@ -149,6 +166,10 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_quant_kernel(NormArg
     const int e0 = (v * NT + t) * VEC;
     const fv w = load_weight<T, VEC>(p.w, p.w_f32, e0, K);
     if (ho != nullptr) store_part<T, VEC>(ho, e0, K, tv[v]);
+    if constexpr (SMALL) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) ss_up += (tv[v][i] * kUp) * (tv[v][i] * kUp);
+    }
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
       ss += tv[v][i] * (tv[v][i] * p.down);
@@ -159,10 +180,12 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_quant_kernel(NormArg
   }
   ss = wave_sum(ss);
   top = wave_max_u32(top);
+  if constexpr (SMALL) ss_up = wave_sum(ss_up);
   if constexpr (W > 1) {
     if ((t & 63) == 0) {
       s_ss[t >> 6] = ss;
       s_top[t >> 6] = top;
+      if constexpr (SMALL) s_up[t >> 6] = ss_up;
     }
     __syncthreads();
     ss = 0.f;
@@ -172,8 +195,13 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_quant_kernel(NormArg
       ss += s_ss[w];
       top = max(top, s_top[w]);
     }
+    if constexpr (SMALL) {
+      ss_up = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) ss_up += s_up[w];
+    }
   }
-  const float rstd = p.norm ? 1.f / sqrtf(ss / ((float)K * p.down) + p.eps) : 1.f;
+  const float rstd = norm_rstd<SMALL>(ss, ss_up, p);
   const bool bad = top >= 0x7F800000u;
   const float amax = __uint_as_float(top);
   const float inv = !bad && amax > kTiny ? 1.f / amax * 127.f : 0.f;
@@ -388,14 +416,14 @@ __global__ __launch_bounds__(1024) void norm_back_join_kernel(const float *part,
 // f16 14.2, 12.8, 16.4).
 int back_groups(int n) { return min(n, 256); }
 
-template <typename T>
+template <typename T, bool SMALL>
 hipError_t norm_quant_of(const NormArgs &a, hipStream_t s) {
   constexpr int VEC = 16 / sizeof(T);
   const int vecs = (a.K - 1) / VEC + 1;   // 16-byte vectors of a row
 #define BMLP_NORM(NT_, R_)                                                                        \
   if (vecs <= NT_ * (R_)) {                                                                       \
     const int rows = NT_ < 256 ? 256 / NT_ : 1;                                                   \
-    hipLaunchKernelGGL((norm_quant_kernel<T, NT_, R_>), dim3((a.n - 1) / rows + 1), dim3(NT_ < 256 ? 256 : NT_), 0, s, a); \
+    hipLaunchKernelGGL((norm_quant_kernel<T, NT_, R_, SMALL>), dim3((a.n - 1) / rows + 1), dim3(NT_ < 256 ? 256 : NT_), 0, s, a); \
     return hipGetLastError();                                                                     \
   }
   BMLP_NORM(64, 1)
@@ -409,6 +437,10 @@ hipError_t norm_quant_of(const NormArgs &a, hipStream_t s) {
   if constexpr (sizeof(T) == 4) BMLP_NORM(1024, 16)
 #undef BMLP_NORM
   return hipErrorInvalidValue;
+}
+template <typename T>
+hipError_t norm_quant_of(const NormArgs &a, hipStream_t s) {
+  return a.norm && a.eps < kSmallMean ? norm_quant_of<T, true>(a, s) : norm_quant_of<T, false>(a, s);
 }
 
 template <typename T, typename TW>
@@ -452,9 +484,7 @@ hipError_t norm_back_of(NormBackArgs &a, hipStream_t s) {
 
 hipError_t launch_norm_quant(int type, const NormArgs &all, hipStream_t s) {
   NormArgs a = all;
-  // squares scaled by a power of two no larger than 1 / K: no rounding of its
-  // own, and the sum stays in range wherever the mean does
-  a.down = 1.f;
+  a.down = 1.f;   // the largest power of two up to 1 / K
   while (a.down * (float)a.K > 1.f) a.down *= 0.5f;
   const int64_t size = type == BMLP_TYPE_F32 ? 4 : 2;
   auto rows_on = [](auto *p, int64_t bytes) {

@@ -9,6 +9,7 @@
 #include <ATen/ATen.h>
 #include <ATen/ops/empty_cuda_dispatch.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -33,12 +34,21 @@ void refuse(const char *format, const char *what) {
   throw PyError{};
 }
 
+// The calls record nothing for autograd: results would leave a tensor's
+// gradient, or its forward-mode tangent, out without a word.
+void no_gradient(const at::Tensor &x, const char *what) {
+  if ((c10::GradMode::is_enabled() && x.requires_grad()) || x._fw_grad(0).defined())
+    refuse("%s requires a gradient, which this call does not record: pass it detached (or call under torch.no_grad()) and "
+           "chain the gradient that norm_quant_backward or distill returns", what);
+}
 const at::Tensor &tensor(PyObject *o, const char *what) {
   if (!THPVariable_Check(o)) {
     PyErr_Format(PyExc_TypeError, "%s must be a tensor", what);
     throw PyError{};
   }
-  return THPVariable_Unpack(o);
+  const at::Tensor &x = THPVariable_Unpack(o);
+  no_gradient(x, what);
+  return x;
 }
 const at::Tensor *tensor_or_none(PyObject *o, const char *what) { return o == Py_None ? nullptr : &tensor(o, what); }
 

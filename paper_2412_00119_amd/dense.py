@@ -10,6 +10,11 @@ binding/dense_binding.cpp; if that module or the library has not been built,
 importing this one raises.  Matrices may be rows cut out of wider ones (a row
 stride); the elements of a row are contiguous.  Arguments that do not fit raise
 ValueError, a status of the library BmlpError.
+
+Nothing here is recorded for autograd.  A tensor that requires a gradient is
+refused while gradients are recorded: pass it detached and chain the gradients
+that ``norm_quant_backward`` and ``distill`` return, for example
+``logits.backward(distill(logits.detach(), ...)[1])``.
 """
 from __future__ import annotations
 
@@ -82,9 +87,10 @@ class QLinear:
     """A layer of 8-bit weights [N][K] with a scale for each of the N outputs.
 
     The weights are laid out for the matrix cores once, here; w itself is not
-    kept.  Inference only: the weights have no gradient."""
+    kept.  Inference only: the layer is made of constants, from parameters too."""
 
     def __init__(self, w, scale, bias=None):
+        scale, bias = scale.detach(), None if bias is None else bias.detach()
         self.packed, = _c.qlinear_pack(w, scale, bias)
         self.n_out, self.n_in = w.shape
         self.scale, self.bias = scale, bias
@@ -92,7 +98,7 @@ class QLinear:
     @classmethod
     def from_weight(cls, w, bias=None):
         """From real-valued weights [N][K], quantised row by row."""
-        return cls(*quantize_rows(w), bias)
+        return cls(*quantize_rows(w.detach()), bias)
 
     def __call__(self, q, scale=None, dtype=torch.bfloat16):
         """q int8 [n][K] with a scale for each row (None: ones) -> [n][N] of dtype."""

@@ -12,6 +12,9 @@
 namespace bmlp {
 namespace {
 
+// a launch holds fewer than 2^32 threads
+constexpr int64_t kMaxThreads = UINT32_MAX;
+
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v16i __attribute__((ext_vector_type(16)));
 
@@ -184,14 +187,25 @@ template <typename T, int S, int NW, int U>
 hipError_t qlinear_direct(const QLinearArgs &a, hipStream_t s) {
   static_assert(S * S / 4 <= 64 * NW, "a thread for four columns");
   const int kblocks = (a.K - 1) / kPackK + 1;
-  const int64_t row_tiles = ((int64_t)a.n - 1) / S + 1, col_tiles = ((int64_t)a.N - 1) / S + 1;
-  if (row_tiles * col_tiles > INT32_MAX) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)(row_tiles * col_tiles));
-  if (ragged(a))
-    hipLaunchKernelGGL((qlinear_direct_kernel<T, S, NW, U, true>), grid, dim3(64 * NW), 0, s, a, kblocks, (int)row_tiles);
-  else
-    hipLaunchKernelGGL((qlinear_direct_kernel<T, S, NW, U, false>), grid, dim3(64 * NW), 0, s, a, kblocks, (int)row_tiles);
-  return hipGetLastError();
+  const int64_t row_tiles = ((int64_t)a.n - 1) / S + 1;
+  // columns of as many launches as their number of threads takes, in whole blocks of weights
+  const int64_t cols = std::max((int64_t)1, kMaxThreads / (64 * NW) / row_tiles * S / kPackRows) * kPackRows;
+  for (int64_t j = 0; j < a.N; j += cols) {
+    QLinearArgs p = a;
+    p.N = (int)std::min(cols, a.N - j);
+    p.w += (size_t)(j / kPackRows) * kblocks * kPackBytes;
+    p.wscale += j;
+    if (p.bias != nullptr) p.bias += j;
+    p.out = static_cast<T *>(a.out) + j;
+    const dim3 grid((unsigned)(row_tiles * (((int64_t)p.N - 1) / S + 1)));
+    if (ragged(a))
+      hipLaunchKernelGGL((qlinear_direct_kernel<T, S, NW, U, true>), grid, dim3(64 * NW), 0, s, p, kblocks, (int)row_tiles);
+    else
+      hipLaunchKernelGGL((qlinear_direct_kernel<T, S, NW, U, false>), grid, dim3(64 * NW), 0, s, p, kblocks, (int)row_tiles);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // ---------------------------------------------------------------------------
@@ -485,7 +499,7 @@ hipError_t qlinear_tiles(const QLinearArgs &a, hipStream_t s) {
   constexpr int TM = 32 * FM * WM, TN = 32 * FN * WN;
   const int kblocks = (a.K - 1) / kPackK + 1, row_tiles = (a.n - 1) / TM + 1, col_tiles = (a.N - 1) / TN + 1;
   const int64_t tiles = (int64_t)row_tiles * col_tiles, per_xcd = (tiles + 7) / 8;
-  if (8 * per_xcd > INT32_MAX || col_tiles > INT32_MAX / 8) return hipErrorInvalidValue;
+  if (8 * per_xcd > kMaxThreads / (64 * WM * WN) || col_tiles > INT32_MAX / 8) return hipErrorInvalidValue;
   // buffer descriptors and their offsets are 32 bits: a tile of q and of w
   if (a.ldq > INT32_MAX / (2 * TM)) return hipErrorInvalidValue;
   const dim3 grid((unsigned)(8 * per_xcd)), block(64 * WM * WN);
@@ -547,11 +561,17 @@ hipError_t qlinear_of(const QLinearArgs &a, hipStream_t s) {
 
 hipError_t launch_qlinear_pack(const int8_t *w, int64_t ldw, int N, int K, uint8_t *packed, hipStream_t s) {
   const int kblocks = (K - 1) / kPackK + 1;
-  const int64_t chunks = (int64_t)((N - 1) / kPackRows + 1) * kblocks * (kPackBytes / 16);
-  if ((chunks - 1) / 256 >= INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(qlinear_pack_kernel, dim3((unsigned)((chunks - 1) / 256 + 1)), dim3(256), 0, s, w, ldw, N, K, kblocks,
-                     chunks, packed);
-  return hipGetLastError();
+  const int64_t block_chunks = (int64_t)kblocks * (kPackBytes / 16);          // of 32 weight rows
+  const int64_t rows = kMaxThreads / 256 * 256 / block_chunks * kPackRows;   // that a launch takes
+  for (int64_t j = 0; j < N; j += rows) {
+    const int n = (int)std::min(rows, N - j);
+    const int64_t chunks = ((int64_t)(n - 1) / kPackRows + 1) * block_chunks;
+    hipLaunchKernelGGL(qlinear_pack_kernel, dim3((unsigned)((chunks - 1) / 256 + 1)), dim3(256), 0, s, w + j * ldw, ldw, n, K,
+                       kblocks, chunks, packed + (size_t)(j / kPackRows) * kblocks * kPackBytes);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_qlinear(int type, const QLinearArgs &all, hipStream_t s) {

@@ -440,7 +440,7 @@ int bmlp_qlinear(int32_t type, int32_t n, int32_t N, int32_t K, const int8_t *d_
  * 0, whatever its logits are.  z = -inf is q = 0.  NaN logits, student's or
  * teacher's, make another row's results NaN.
  * 2 <= c <= BMLP_MAX_DISTILL_CLASSES, 1 <= k <= BMLP_MAX_DISTILL_LISTED,
- * tau > 0 and finite. */
+ * tau > 0 and finite, and so is log2(e) / tau (tau >= 4.3e-39). */
 int bmlp_distill(int32_t type, int32_t n, int32_t c, const void *d_z, int64_t ldz, int32_t k, const int32_t *d_idx,
                  const void *d_t, int32_t t_type, const float *d_lse, const float *d_weight, float tau, float *d_loss,
                  void *d_dz, int64_t lddz, void *stream);

@@ -126,7 +126,8 @@ int bmlp_qlinear(int32_t type, int32_t n, int32_t N, int32_t K, const int8_t *d_
 int bmlp_distill(int32_t type, int32_t n, int32_t c, const void *d_z, int64_t ldz, int32_t k, const int32_t *d_idx,
                  const void *d_t, int32_t t_type, const float *d_lse, const float *d_weight, float tau, float *d_loss,
                  void *d_dz, int64_t lddz, void *stream) {
-  if (!type_ok(type) || !type_ok(t_type) || !(tau > 0.f) || !isfinite(tau)) return BMLP_EINVAL;
+  // the kernel multiplies by log2(e) / tau
+  if (!type_ok(type) || !type_ok(t_type) || !(tau > 0.f) || !isfinite(tau) || !isfinite(1.44269504f / tau)) return BMLP_EINVAL;
   if (n < 0 || c < 2 || c > BMLP_MAX_DISTILL_CLASSES || k < 1 || k > BMLP_MAX_DISTILL_LISTED) return BMLP_ESHAPE;
   if (n == 0) return BMLP_OK;
   if (!rows_ok(d_z, ldz, n, c, type_size(type)) || !f32_ok(d_idx) || !rows_ok(d_t, k, n, k, type_size(t_type)) ||

@@ -7,8 +7,10 @@
 // the zeros past K in them make whatever is read past the end of a row of q
 // harmless.
 #include "dense.h"
+#include "qlinear_plan.h"
 
 #include <algorithm>
+
 namespace bmlp {
 namespace {
 
@@ -41,10 +43,7 @@ __global__ __launch_bounds__(256) void qlinear_pack_kernel(const int8_t *w, int6
   __builtin_memcpy(__builtin_assume_aligned(packed + 16 * i, 16), b, 16);
 }
 
-// Rows of q that do not start (or, for the last one, end) at 16-byte boundaries.
-bool ragged(const QLinearArgs &a) {
-  return ((reinterpret_cast<uintptr_t>(a.q) | (a.n > 1 ? (uintptr_t)a.ldq : 0) | (uintptr_t)a.K) & 15) != 0;
-}
+bool ragged(const QLinearArgs &a) { return qlinear_ragged(reinterpret_cast<uintptr_t>(a.q), a.n, a.ldq, a.K); }
 
 // 16 bytes of row i at byte k: past K they are not used (the packed weights
 // are zero there), so reading on into the next row is fine, past the last
@@ -512,47 +511,15 @@ hipError_t qlinear_tiles(const QLinearArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Which kernel.  Up to 32 rows the weights' bytes count and the direct kernel
-// streams them (us; 16 rows, 8192 x 8192: 12.6 in 32 x 32 tiles, 13.3 in 16 x 16
-// ones, 26 through LDS; 4096 x 4096, where 16 x 16 tiles find every compute unit: 7.3 and
-// 7.8, 14.4).  Above, the tile whose rounds over the 256 compute units cost
-// least: 256 x 256 tiles run the matrix cores at their highest rate, smaller
-// ones find more compute units.  Measured, us, 256 x 256 / 128 x 256 / 128 x 128
-// / 64 x 128 / 64 x 64: 4096 x 4096 x 4096 66, 70, 82, 103, 114; 2048 x 4096 x 4096
-// 44, 36, 42, 52, 57; 1024 x 4096 x 4096 42, 25, 22, 26, 31; 512 x 4096 x 4096 41,
-// 24, 19, 14.5, 17.4; 256 x 4096 x 4096 41, 24, 18, 13, 10; 8192 x 1024 x 1024 20,
-// 14.5, 18, 22, 22; 3000 x 8192 x 3000 82, 103, 104, 114, 130.
-struct TileCost {
-  int rows, cols, units;   // units: tiles that run at a time
-  int full, least;         // ns per step of 64 inputs: all units busy (the clock falls then), and few of them
-};
-constexpr TileCost kTileCost[5] = {
-    {256, 256, 256, 1000, 640}, {128, 256, 256, 560, 385}, {128, 128, 256, 344, 295}, {64, 128, 256, 226, 200}, {64, 64, 512, 270, 145}};
-int best_tile(int n, int N) {
-  int best = 0;
-  int64_t lowest = INT64_MAX;
-  for (int i = 0; i < 5; ++i) {
-    const TileCost &c = kTileCost[i];
-    const int64_t t = (int64_t)((n - 1) / c.rows + 1) * ((N - 1) / c.cols + 1), rest = t % c.units;
-    const int64_t cost = t / c.units * c.full + (rest ? std::max((int64_t)c.least, c.full * rest / c.units) : 0);
-    if (cost < lowest) {
-      lowest = cost;
-      best = i;
-    }
-  }
-  return best;
-}
-
 template <typename T>
 hipError_t qlinear_of(const QLinearArgs &a, hipStream_t s) {
-  if (a.n <= 16 && a.N < 8192) return qlinear_direct<T, 16, 8, 4>(a, s);
-  // (rows too far apart for a tile's 32-bit offsets: the direct kernel's are 64)
-  if (a.n <= 32 || a.ldq > 1 << 21) return qlinear_direct<T, 32, 16, 2>(a, s);
-  switch (best_tile(a.n, a.N)) {
-    case 0: return qlinear_tiles<T, 4, 2, 2, 4, 4>(a, s);
-    case 1: return qlinear_tiles<T, 2, 2, 2, 4, 4>(a, s);
-    case 2: return qlinear_tiles<T, 2, 2, 2, 2, 8>(a, s);
-    case 3: return qlinear_tiles<T, 1, 2, 2, 2, 8>(a, s);
+  switch (qlinear_kernel(a.n, a.N, a.ldq)) {
+    case kDirect16: return qlinear_direct<T, 16, 8, 4>(a, s);
+    case kDirect32: return qlinear_direct<T, 32, 16, 2>(a, s);
+    case kTile256x256: return qlinear_tiles<T, 4, 2, 2, 4, 4>(a, s);
+    case kTile128x256: return qlinear_tiles<T, 2, 2, 2, 4, 4>(a, s);
+    case kTile128x128: return qlinear_tiles<T, 2, 2, 2, 2, 8>(a, s);
+    case kTile64x128: return qlinear_tiles<T, 1, 2, 2, 2, 8>(a, s);
     default: return qlinear_tiles<T, 1, 1, 2, 2, 8>(a, s);
   }
 }

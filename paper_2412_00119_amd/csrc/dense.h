@@ -69,13 +69,7 @@ constexpr int kRowsPerLaunch = 1 << 20;
 template <typename T, int N>
 using vec_t = T __attribute__((ext_vector_type(N)));
 
-// N values at p, which is aligned to a value only
-template <typename T, int N>
-__device__ __forceinline__ vec_t<float, N> load_f32(const T *p) {
-  vec_t<T, N> v;
-  __builtin_memcpy(&v, p, sizeof(v));
-  return __builtin_convertvector(v, vec_t<float, N>);
-}
+// N values to p, which is aligned to a value only
 template <typename T, int N>
 __device__ __forceinline__ void store_as(T *p, const vec_t<float, N> &f) {
   const vec_t<T, N> v = __builtin_convertvector(f, vec_t<T, N>);

@@ -460,8 +460,11 @@ hipError_t norm_back_of(NormBackArgs &a, hipStream_t s) {
   BMLP_NORM(256, 1, 4)
   BMLP_NORM(512, 1, 2)
   BMLP_NORM(1024, 1, 1)
-  if constexpr (sizeof(T) == 4) BMLP_NORM(1024, 2, 1)   // (16-bit rows: spills)
-  BMLP_NORM(512, 4, 1)
+  if constexpr (sizeof(T) == 4) {
+    BMLP_NORM(1024, 2, 1)
+  } else {
+    BMLP_NORM(512, 4, 1)
+  }
 #undef BMLP_NORM
 #define BMLP_NORM(R_)                                                                             \
   if (vecs <= 1024 * R_) {                                                                        \

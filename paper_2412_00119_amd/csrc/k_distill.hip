@@ -15,7 +15,8 @@
 // are listed is a bit per position in LDS; a vector's listed places become -inf,
 // so that they drop out of maximum, sum and gradient alike, and their gradients
 // are written at the end.  The first wave works on the list (teacher's softmax,
-// the listed part of L, the loss) while the others sum.
+// the listed part of L, the loss) while the others sum; where a row has one wave
+// only, before it sums.
 //
 // What bounds it: 4 bytes of traffic a class in 16 bits, and two exponentials
 // a class at a quarter of the vector rate.  2048 x 131072 bf16 (1.07 GB): 254 us, 4.2

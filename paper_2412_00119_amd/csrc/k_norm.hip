@@ -8,13 +8,15 @@
 // what follows needs t alone, which stays in registers: every input is read
 // once and every output written once.  |t| is compared as its bits, an order in
 // which NaN and infinity come last and so are not lost.  8192 x 4096 bf16 with
-// residual and values (302 MB): 55 us, 5.5 TB/s, more than a large copy reaches.
+// residual and values (302 MB): 55 us a pass among others, 5.5 TB/s, where a large
+// copy reaches 4.9.  Rows above 32768 spill: 2048 x 32768 bf16 123 us, but 1024 x
+// 40000 1046 and 1024 x 65536 1076 (f16 867, f32 273).
 //
 // Backward.  dx needs one sum per row, of g h with g = dy w; dweight needs one
 // sum per column over all rows.  A work-group keeps its columns' sums in
 // registers over the rows it walks and writes them once; a second launch adds
-// the work-groups' sums in a fixed order.  4096 x 8192 bf16 (268 MB): 48 us, 5.5
-// TB/s, both launches.
+// the work-groups' sums in a fixed order.  4096 x 8192 bf16 (268 MB): 52.5 us a pass
+// among others, 5.1 TB/s (43 and 4 of it the kernels, alone).
 //
 // Rounding: h, dx and y are rounded to their type once, from 32 bits; q to whole
 // numbers, half to even; the scale is what it is in 32 bits.
@@ -339,7 +341,11 @@ __global__ __launch_bounds__(NT *G) void norm_back_kernel(NormBackArgs p) {
 }
 
 // The widest rows: only the columns' sums stay in registers, a row is read again
-// for dx.  (1024 x 32768 bf16: 741 us with rows and weights held, which spills.)
+// for dx.  Its registers spill all the same (16-bit rows 26-34 up to 32768 wide,
+// 172-269 above; 32-bit rows 80 up to 32768 wide, 314 above), much less than with
+// rows and weights held (1024 x 32768 bf16 741 us).  us a call with dh and dweight:
+// bf16 2048 x 20000 125, 1024 x 32768 103, 1024 x 65536 450; f32 4096 x 16384 241,
+// 1024 x 32768 204, 1024 x 65536 664: 1.2 to 4.5 TB/s.
 template <typename T, typename TW, int R>
 __global__ __launch_bounds__(1024) void norm_back_wide_kernel(NormBackArgs p) {
   constexpr int VEC = 16 / sizeof(T), NT = 1024;
@@ -416,6 +422,20 @@ __global__ __launch_bounds__(1024) void norm_back_join_kernel(const float *part,
 // f16 14.2, 12.8, 16.4).
 int back_groups(int n) { return min(n, 256); }
 
+// Shape by the vectors of a row, measured with residual, h and y, us, bf16 / f32 rows
+// of that many, the one taken first:
+//   16384 rows of 60   64 x 1 14.1 / 12.5, 256 x 1 29.9 / 21.8
+//   16384 rows of 128  64 x 2 24.2 / 22.6, 256 x 1 29.9 / 25.3
+//   8192 rows of 129   256 x 1 17.4 / 15.6, 64 x 3 14.3 / 13.4
+//   8192 rows of 256   256 x 1 24.5 / 23.1, 64 x 4 24.8 / 22.5
+//   8192 rows of 300   256 x 2 29.1 / 27.9, 64 x 8 35.8 / 29.3, 512 x 1 29.6 / 27.3
+//   8192 rows of 512   256 x 2 49.2 / 53.3, 64 x 8 58.7 / 48.3, 512 x 1 48.8 / 51.2
+//   8192 rows of 1024  256 x 4 111 / 109, 512 x 2 109 / 104, 1024 x 1 107 / 106
+//   4096 rows of 1500  512 x 4 85.5 / 84.7, 256 x 8 91.1 / 92.0, 1024 x 2 85.1 / 80.7
+//   4096 rows of 2048  512 x 4 114 / 110, 256 x 8 118 / 112, 1024 x 2 115 / 106
+//   2048 rows of 4096  1024 x 4 122 / 113, 512 x 8 130 / 119
+//   300 rows of 512    256 x 2 4.9 / 4.2, 64 x 8 8.8 / 8.1, 512 x 1 4.7 / 4.2
+// What is wider has no other shape that fits a work-group.
 template <typename T, bool SMALL>
 hipError_t norm_quant_of(const NormArgs &a, hipStream_t s) {
   constexpr int VEC = 16 / sizeof(T);
@@ -460,6 +480,8 @@ hipError_t norm_back_of(NormBackArgs &a, hipStream_t s) {
   BMLP_NORM(256, 1, 4)
   BMLP_NORM(512, 1, 2)
   BMLP_NORM(1024, 1, 1)
+  // 4096 x 16384 bf16: 512 x 4, which spills 30-42 registers, 112 us; 1024 x 2 520; rows
+  // read twice 124.  4096 x 12288: 85, 495, 102
   if constexpr (sizeof(T) == 4) {
     BMLP_NORM(1024, 2, 1)
   } else {

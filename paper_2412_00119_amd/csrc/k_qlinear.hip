@@ -92,8 +92,10 @@ __device__ __forceinline__ v4i bytes_of(const Words &w, const int8_t *p) {
 // taking the 64-input blocks in turn (wave w blocks w, w + NW, ...), U of them
 // in flight at a time, operands straight from memory; the waves' sums are
 // joined in LDS.  S is the MFMA's size, 16 (one MFMA a block) or 32 (two).  The
-// weights are read once from memory, 16 rows of 8192 inputs against 8192 weight
-// rows (67 MB) in 12.5 us, 5.4 TB/s: what bounds it.
+// weights' bytes bound it, each read once: 16 rows of 8192 inputs against 8192
+// weight rows (67 MB) in 12.5 us, 5.4 TB/s, where the weights are still in the
+// last-level cache from the call before, and 16.1 us, 4.2 TB/s, over twelve layers in
+// turn (805 MB), which that cache does not hold.
 // ---------------------------------------------------------------------------
 template <typename T, int S, int NW, int U, bool RAGGED>
 __global__ __launch_bounds__(64 * NW) void qlinear_direct_kernel(QLinearArgs p, int kblocks, int row_tiles) {
@@ -219,7 +221,7 @@ hipError_t qlinear_direct(const QLinearArgs &a, hipStream_t s) {
 // issued between MFMAs too.  Where rows of q do not start at 16-byte boundaries
 // (RAGGED) they go through registers instead.
 //
-// What bounds it.  Large products: the card's power.  8192^3 in 465 us, 2360 TOP/s:
+// What bounds it.  Large products: the card's power.  8192^3 in 468 us, 2350 TOP/s:
 // the matrix cores are busy for 76% of the cycles, at 1.5 GHz instead of 2.4; a
 // loop of the same MFMAs on random operands that stay in registers reaches 3300
 // to 3450 (at full issue and 1.6 GHz), the library's product 2070.  Few tiles:

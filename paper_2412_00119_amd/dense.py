@@ -90,15 +90,16 @@ class QLinear:
     kept.  Inference only: the layer is made of constants, from parameters too."""
 
     def __init__(self, w, scale, bias=None):
-        scale, bias = scale.detach(), None if bias is None else bias.detach()
-        self.packed, = _c.qlinear_pack(w, scale, bias)
+        with torch.no_grad():
+            self.packed, = _c.qlinear_pack(w, scale, bias)
         self.n_out, self.n_in = w.shape
-        self.scale, self.bias = scale, bias
+        self.scale, self.bias = scale.detach(), None if bias is None else bias.detach()
 
     @classmethod
     def from_weight(cls, w, bias=None):
         """From real-valued weights [N][K], quantised row by row."""
-        return cls(*quantize_rows(w.detach()), bias)
+        with torch.no_grad():
+            return cls(*quantize_rows(w), bias)
 
     def __call__(self, q, scale=None, dtype=torch.bfloat16):
         """q int8 [n][K] with a scale for each row (None: ones) -> [n][N] of dtype."""

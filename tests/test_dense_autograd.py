@@ -83,3 +83,11 @@ def test_chained_by_hand():
     p = torch.zeros(4, 6, dtype=torch.float64).scatter(1, idx.long(), torch.softmax(t.double(), 1))
     (-p * torch.log_softmax(a.double() @ want, 1)).sum().backward()
     assert ((on_gpu.grad.cpu().double() - want.grad).abs() <= 4 * 4 * 512 * 2.0 ** -24).all()
+
+
+def test_layer_of_what_is_no_tensor():
+    w = torch.ones((4, 8), dtype=torch.int8)
+    for call in (lambda: D.QLinear(w, None), lambda: D.QLinear(None, R), lambda: D.QLinear(w, 1.0), lambda: D.QLinear.from_weight(None),
+                 lambda: D.QLinear.from_weight([[1.0]])):
+        with pytest.raises((TypeError, ValueError)):   # (ValueError: w is not on the GPU)
+            call()
